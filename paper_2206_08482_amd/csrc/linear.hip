@@ -37,15 +37,15 @@ __device__ __forceinline__ float sigmoid_of(float z) {
   const float d = 1.f + exp_of<EXACT>(-z);
   return EXACT ? 1.f / d : __builtin_amdgcn_rcpf(d);
 }
-// Phi(z).  Not EXACT: 1 - Phi(|z|) = phi-weighted polynomial of t = 1 / (1 + p |z| / sqrt 2), Abramowitz and Stegun 7.1.26
-// (error of erf 1.5e-7).
+// Phi(z).  Not EXACT: 1 - Phi(|z|) = e^(-z^2 / 2) t P(t) with t = 1 / (1 + 0.294 |z|) and P of degree 5, fitted to erfcx (alternately reweighted least
+// squares, |z| up to 13.2) so that it is right to 2.5e-7 of 1 and to 4e-5 of itself: GELU's far negative values are as right as its others.
 template <bool EXACT>
 __device__ __forceinline__ float normal_cdf(float z) {
   if constexpr (EXACT) return 0.5f * erfcf(-0.70710678f * z);
-  const float x = fabsf(z) * 0.70710678f;
-  const float t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * x);
-  const float poly = ((((1.061405429f * t - 1.453152027f) * t + 1.421413741f) * t - 0.284496736f) * t + 0.254829592f) * t;
-  const float tail = 0.5f * poly * exp_of<false>(-x * x);
+  const float t = __builtin_amdgcn_rcpf(1.f + 0.29415643f * fabsf(z));
+  const float poly =
+      (((((-0.0848032236f * t + 0.257211983f) * t - 0.0609185249f) * t + 0.163766786f) * t + 0.106596917f) * t + 0.118145958f) * t;
+  const float tail = poly * __builtin_amdgcn_exp2f(z * z * -0.72134752f);
   return z < 0.f ? tail : 1.f - tail;
 }
 
