@@ -329,8 +329,8 @@ int adam_update(gmi_t gmi, float* params, float* adam_m, float* adam_v, const fl
  *   backward  dz = dy * act'(pre),  dx = dz w,  dw = dz^T x,  dbias = sum over rows of dz   (the residual's gradient is dy itself)
  * dtype BF16: x, w, residual, y, pre, dy, dx, dw are bf16, products on matrix cores with fp32 sums, everything up to the output in fp32
  * but for dz, which is rounded to bf16 once before the two products that read it.  dtype F32: all fp32; products of three bf16 planes
- * per operand (24 bits of significand, six products) with fp32 sums; an infinite operand gives infinity or NaN.  bias and dbias are
- * fp32 for both (dbias sums the unrounded dz).
+ * per operand (24 bits of significand, six products) with fp32 sums; infinities and NaN give what an fp32 product gives
+ * (but an infinity times a value below 2^-126 may give NaN).  bias and dbias are fp32 for both (dbias sums the unrounded dz).
  * Shapes: x [n_rows, in_dim], w [out_dim, in_dim] (grouped: [n_groups, out_dim, in_dim]), bias [out_dim] ([n_groups, out_dim]),
  * y, pre, residual, dy [n_rows, out_dim], dx as x, dw as w, dbias as bias; w, bias, dw, dbias contiguous, the others with a row pitch
  * ld* (elements, >= the row's length).  Any pitch and any element-aligned address is right; 16-byte aligned rows whose length is a

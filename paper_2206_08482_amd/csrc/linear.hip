@@ -389,7 +389,7 @@ __device__ __forceinline__ void product_block(const ProductArgs& a, int block, c
   Q.ld = a.q_ld; Q.plane = a.q_plane; Q.count = m_end - m0;
   Q.base = a.q + (QS ? (int64_t)k0 * a.q_ld + (int64_t)m0 * 2 : (int64_t)m0 * a.q_ld + (int64_t)k0 * 2);
   Accumulator<S> acc;
-  multiply<S, PS, QS, false, FORM == kForwardRaw>(P, Q, k_len, a.pairs, smem, acc);
+  multiply<S, PS, QS, false, FORM == kForwardRaw, F32>(P, Q, k_len, a.pairs, smem, acc);
 
   if (a.splits > 1) {
     const int pitch = (a.cols + 7) & ~7;

@@ -261,6 +261,20 @@ struct Walk {
   }
 };
 
+// Between the smaller products of planes and the first planes' own (the last pair).  An infinite value is its first plane alone, the others are 0, and the
+// planes of what it meets have signs of their own: the smaller products would make NaN of it.  The first planes' product decides: infinities and NaN of
+// the sums so far are dropped, what they come from is in it again.
+// (In a loop over both parts: a branch around it within the loop over stages takes 3 to 6 % of the time.)
+template <class S>
+__device__ __forceinline__ void keep_finite(Accumulator<S>& acc) {
+#pragma unroll
+  for (int i = 0; i < S::RN; ++i)
+#pragma unroll
+    for (int j = 0; j < S::RM; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc.v[i][j][e] = __builtin_amdgcn_classf(acc.v[i][j][e], 0x207) ? 0.f : acc.v[i][j][e];      // NaN, infinities
+}
+
 template <bool HALF>
 __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c) {
   if constexpr (HALF) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
@@ -274,7 +288,7 @@ __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c) {
 // are read in the shadow of the one before it.  After the first phase everything of half 0 and of Q is in registers, after the third
 // everything of half 1: there the workgroup's waves meet, and the place takes the stage R later, which is loaded two or more phases before it
 // is next waited for.
-template <class S, bool PS, bool QS, bool HALF>
+template <class S, bool PS, bool QS, bool HALF, bool INFINITE>
 __device__ __forceinline__ void multiply_shared(const Side& P, const Side& Q, int k_len, Pairs pairs, char* smem, Accumulator<S>& acc) {
   constexpr int H = S::H, RM = S::RM, kSteps = H * RM;
   static_assert((!PS || 64 % (S::half / 8) == 0) && (!QS || 64 % (S::TM / 8) == 0), "a strided side's rows have to fill a piece");
@@ -351,31 +365,42 @@ __device__ __forceinline__ void multiply_shared(const Side& P, const Side& Q, in
   uint32_t cur = 0;
 #pragma unroll
   for (int t = 0; t < kSteps; ++t) read_both(t, 0, 0, pa, qa);
-  for (int st = 0; st < n; ++st) {
-    const uint32_t next = cur == (S::R - 1) * S::stage ? 0 : cur + S::stage;
-    phase(0, pa, qa, [&](int t) { read_both(t, cur, 1, pb, qb); });
-    wait_and_meet<(S::R - 1) * S::pieces>();      // half 1 of this stage has landed; half 0 and Q have been read
-    phase(0, pb, qb, [&](int t) {
-      read_p(t, cur + S::half_bytes, 0, pa);
-      if (t == kSteps / 2) load_p0(cur);
-    });
-    phase(H, pa, qa, [&](int t) {
-      read_p(t, cur + S::half_bytes, 1, pb);
-      if (t == kSteps / 2) load_q(cur);
-    });
-    wait_and_meet<(S::R - 1) * S::pieces>();      // half 0 and Q of the next stage have landed; half 1 has been read
-    phase(H, pb, qb, [&](int t) {
-      read_both(t, next, 0, pa, qa);
-      if (t == kSteps / 2) load_p1(cur);
-    });
-    cur = next;
+  auto stages = [&](int count) {
+    for (int st = 0; st < count; ++st) {
+      const uint32_t next = cur == (S::R - 1) * S::stage ? 0 : cur + S::stage;
+      phase(0, pa, qa, [&](int t) { read_both(t, cur, 1, pb, qb); });
+      wait_and_meet<(S::R - 1) * S::pieces>();      // half 1 of this stage has landed; half 0 and Q have been read
+      phase(0, pb, qb, [&](int t) {
+        read_p(t, cur + S::half_bytes, 0, pa);
+        if (t == kSteps / 2) load_p0(cur);
+      });
+      phase(H, pa, qa, [&](int t) {
+        read_p(t, cur + S::half_bytes, 1, pb);
+        if (t == kSteps / 2) load_q(cur);
+      });
+      wait_and_meet<(S::R - 1) * S::pieces>();      // half 0 and Q of the next stage have landed; half 1 has been read
+      phase(H, pb, qb, [&](int t) {
+        read_both(t, next, 0, pa, qa);
+        if (t == kSteps / 2) load_p1(cur);
+      });
+      cur = next;
+    }
+  };
+  if constexpr (INFINITE) {
+#pragma unroll 1
+    for (int part = 0; part < 2; ++part) {
+      keep_finite<S>(acc);      // before the first part as well, where it changes nothing: only between them, Large spills registers
+      stages(part ? n / pairs.n : n - n / pairs.n);
+    }
+  } else {
+    stages(n);
   }
   wait_and_meet<0>();
 }
 
 // The same for an OwnShape: every wave ends with its part of the tile's sums.
 // RAW: both sides contiguous, at any address (one plane).
-template <class S, bool PS, bool QS, bool HALF, bool RAW>
+template <class S, bool PS, bool QS, bool HALF, bool RAW, bool INFINITE>
 __device__ __forceinline__ void multiply_own(const Side& P, const Side& Q, int k_len, Pairs pairs, char* smem, Accumulator<S>& acc) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t base = wave * S::ring, lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem + base;
@@ -445,30 +470,43 @@ __device__ __forceinline__ void multiply_own(const Side& P, const Side& Q, int k
     if constexpr (!RAW) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S::R - 1) * S::pieces) : "memory");
     int slot = 0;
     read(0, 0, p0, q0);
-    for (int st = 0; st < n; ++st) {
-      if constexpr (RAW) load(slot);      // the stage R later, on its way to registers while this one is multiplied
-      read(slot * S::stage, 1, p1, q1);
-      product(p0, q0);
-      const int done = slot;
-      slot = slot == S::R - 1 ? 0 : slot + 1;
-      if constexpr (!RAW) {
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // the slot has been read: it takes the stage R later
-        load(done);
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S::R - 1) * S::pieces) : "memory");
+    auto stages = [&](int count) {
+      for (int st = 0; st < count; ++st) {
+        if constexpr (RAW) load(slot);      // the stage R later, on its way to registers while this one is multiplied
+        read(slot * S::stage, 1, p1, q1);
+        product(p0, q0);
+        const int done = slot;
+        slot = slot == S::R - 1 ? 0 : slot + 1;
+        if constexpr (!RAW) {
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // the slot has been read: it takes the stage R later
+          load(done);
+          asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S::R - 1) * S::pieces) : "memory");
+        }
+        read(slot * S::stage, 0, p0, q0);
+        product(p1, q1);
+        put(done);
       }
-      read(slot * S::stage, 0, p0, q0);
-      product(p1, q1);
-      put(done);
+    };
+    if constexpr (INFINITE) {
+      const int before = min(n, max(0, (total - per_pair - wave + S::W - 1) / S::W));      // this wave's stages before the last pair
+#pragma unroll 1
+      for (int part = 0; part < 2; ++part) {
+        stages(part ? n - before : before);
+        if (part == 0) keep_finite<S>(acc);
+      }
+    } else {
+      stages(n);
     }
   }
   asm volatile("s_waitcnt vmcnt(0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
-template <class S, bool PS, bool QS, bool HALF, bool RAW = false>
+// INFINITE: operands in several planes may hold infinities.
+template <class S, bool PS, bool QS, bool HALF, bool RAW = false, bool INFINITE = false>
 __device__ __forceinline__ void multiply(const Side& P, const Side& Q, int k_len, Pairs pairs, char* smem, Accumulator<S>& acc) {
   static_assert(!RAW || IsOwn<S>::value, "");
-  if constexpr (IsOwn<S>::value) multiply_own<S, PS, QS, HALF, RAW>(P, Q, k_len, pairs, smem, acc);
-  else multiply_shared<S, PS, QS, HALF>(P, Q, k_len, pairs, smem, acc);
+  if constexpr (IsOwn<S>::value) multiply_own<S, PS, QS, HALF, RAW, INFINITE>(P, Q, k_len, pairs, smem, acc);
+  else multiply_shared<S, PS, QS, HALF, INFINITE>(P, Q, k_len, pairs, smem, acc);
 }
 
 // What the functions below hand out with the sums: fetch(m, n) is called ahead of row(m, n, v, what it gave), for several rows at a time, so that
