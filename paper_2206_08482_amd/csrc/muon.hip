@@ -3,8 +3,10 @@
 // Every matrix is held with its shorter side p as rows (X [p, q], transposed on the way in and out if it is taller than wide), so that
 // each step is three products, batched over all bound matrices: S = X X^T and B = t (a I + b t^2 S + c t^4 S^2), both symmetric (tiles on
 // and below the diagonal are computed and mirrored), then X <- B X.  The a X term rides on B's diagonal, so the last product needs no
-// epilogue operand.  X starts as G 2^-e, exact in fp16 for bf16 gradients, with |X| <= 1; what is left of 1 / (|G| + eps) is the
-// factor t in 1 .. 2 that the first step's B carries.
+// epilogue operand.  X starts as G 2^-e with |X| in 1/2 .. 1, e from |G| alone; what is left of 1 / (|G| + eps) is the factor t (in 1 .. 2 unless eps
+// counts) that the first step's B carries.  Where t is so small that it would leave nothing of X in fp16, it goes into X step by step: carry_of.
+// A bf16 gradient is held exactly by one plane of 11 bits (down to 2^-26 of the norm).  muon_update's direction u is fp32 and is rounded to those
+// 11 bits, once, with bf16 gradients: 2^-12 of it, beside the 2^-9 that the gradient itself was rounded to.
 //
 // Powers of two keep the fp16 values away from the ends of the type: entries of X and S reach 1 and may be as small as 1 / sqrt(p q).
 #include <numeric>
@@ -47,7 +49,7 @@ struct gmi_muon {
   char* base;
   Entry* table;             // device
   double* sums;             // [chunks]
-  float* factor;            // [n] t
+  float* factor;            // [n] t: 1 / (|G| + eps) is t 2^-e
   float* part;
   std::vector<Entry> host;
   int64_t length;           // the flat vectors reach at least here
@@ -70,11 +72,28 @@ struct MuonArgs {
   float *moments_out, *params_out;
   void* dst;
   float momentum, a, b, c, eps, lr, decay;
-  int nesterov, first, last, from, to;      // of a step: X[from] -> X[to]
+  int nesterov, step, last, from, to;       // of a step: X[from] -> X[to]
   int tile0, splits;                        // of the launch: place of its first tile in the running count
   float* part;                              // sums of splits, 64 x 64 of each workgroup
   Entry only;                               // the table's first
 };
+
+// The matrix that a step starts from is X = at Y, Y being what the planes hold, and the step's B carries the factor `with`: Y <- with (a I + b at^2 S +
+// c at^4 S^2) Y.  In step 0 at = t.  A t of at least 1 goes into Y at once, and so does one that then leaves Y no smaller than it was; otherwise Y
+// keeps its size (with = 1 / the most that a step lengthens X by where |X| <= at) and the growth goes to `at`.
+struct Carry { float at, with; };
+__device__ __forceinline__ Carry carry_of(const MuonArgs& a, float t, int step) {
+  Carry c = {t, t};
+  for (int k = 0; c.at < 1.f; ++k) {
+    const float s = c.at * c.at, most = fmaxf(1.f, fabsf(a.a) + s * (fabsf(a.b) + s * fabsf(a.c)));
+    const bool all = c.at * most >= 1.f;
+    c.with = all ? c.at : 1.f / most;
+    if (k == step) return c;
+    if (all) break;
+    c.at *= most;
+  }
+  return step == 0 ? c : Carry{1.f, 1.f};
+}
 
 // The entry that holds place `i` of a running count, `first`: where an entry begins in it.  Every kernel's caches start empty, and a step has
 // three launches of a few us each: a table in memory costs two trips one after the other before the first operand is asked for, so the
@@ -208,12 +227,11 @@ __global__ __launch_bounds__(256) void muon_pack_kernel(MuonArgs a) {
   }
   double sum = 0.0;
   for (int i = threadIdx.x; i < E.chunks; i += 256) sum += a.sums[E.first_chunk + i];
-  sum = block_sum(sum, lds);
-  const float norm = (float)(sqrt(sum) + a.eps);
+  const double norm = sqrt(block_sum(sum, lds));      // of finite values finite
   int ex;
-  (void)frexpf(norm, &ex);
-  if (!(norm < INFINITY)) ex = 0;
-  if (local == 0 && threadIdx.x == 0) a.factor[e] = norm < INFINITY ? ldexpf(1.f, ex) / norm : NAN;
+  (void)frexp(norm, &ex);
+  if (!(norm > 0.0 && norm < INFINITY)) ex = 0;
+  if (local == 0 && threadIdx.x == 0) a.factor[e] = !(norm < INFINITY) ? NAN : norm > 0.0 ? (float)(ldexp(1.0, ex) / (norm + a.eps)) : 1.f;
 #pragma unroll
   for (int k = 0; k < 16; ++k) u[k] = ldexpf(u[k], kScaleX - ex);
   constexpr int PLANES = F32 ? 2 : 1;
@@ -280,6 +298,7 @@ __global__ __launch_bounds__(S::threads, kWavesPerSimd<S>) void muon_symmetric_k
     P.base += k0 * 2;
     Q.base += k0 * 2;
   }
+  const float t0 = SQUARE ? a.factor[e] : 1.f;      // asked for here, so that it is there at the end
   Accumulator<S> acc;
   multiply<S, false, false, true>(P, Q, k_len, F32 ? kTwoPlanes : kOnePlane, smem, acc);
   if (divided && splits > 1) {
@@ -288,9 +307,9 @@ __global__ __launch_bounds__(S::threads, kWavesPerSimd<S>) void muon_symmetric_k
     return;
   }
 
-  const float t = SQUARE && a.first ? a.factor[e] : 1.f;
-  const float ta = t * a.a * (1 << kScaleB), tb = t * t * t * a.b * ldexpf(1.f, kScaleB - kScaleS),
-              tc = t * t * t * t * t * a.c * ldexpf(1.f, kScaleB - 2 * kScaleS), ts = ldexpf(1.f, kScaleS - 2 * kScaleX);
+  const Carry t = SQUARE ? carry_of(a, t0, a.step) : Carry{1.f, 1.f};
+  const float ta = t.with * a.a * (1 << kScaleB), tb = t.with * t.at * t.at * a.b * ldexpf(1.f, kScaleB - kScaleS),
+              tc = t.with * t.at * t.at * t.at * t.at * a.c * ldexpf(1.f, kScaleB - 2 * kScaleS), ts = ldexpf(1.f, kScaleS - 2 * kScaleX);
   const char* s = a.base + E.s;
   char* out = a.base + (SQUARE ? E.b : E.s);
   // eight values of row m at columns n ..: S there, and what is made of the sums v
@@ -376,6 +395,7 @@ __global__ __launch_bounds__(S::threads, kWavesPerSimd<S>) void muon_apply_kerne
   Side P, Q;
   P.ld = 2 * (int64_t)E.qp; P.plane = E.x_plane; P.base = a.base + (a.from ? E.x[1] : E.x[0]) + n0 * 2; P.count = min(T, E.q - n0);
   Q.ld = 2 * (int64_t)E.pp; Q.plane = E.s_plane; Q.base = a.base + E.b + m0 * Q.ld; Q.count = min(T, E.p - m0);
+  const float t0 = a.last ? a.factor[e] : 1.f;
   Accumulator<S> acc;
   multiply<S, true, false, true>(P, Q, E.p, F32 ? kTwoPlanes : kOnePlane, smem, acc);
 
@@ -390,7 +410,7 @@ __global__ __launch_bounds__(S::threads, kWavesPerSimd<S>) void muon_apply_kerne
     });
     return;
   }
-  const float scale = ldexpf(1.f, -kScaleB - kScaleX);
+  const float scale = carry_of(a, t0, a.step + 1).at * ldexpf(1.f, -kScaleB - kScaleX);
   const float step = a.lr * sqrtf(fmaxf(1.f, (float)E.rows / (float)E.cols));
   // eight values of row r of the matrix at columns c ..: its parameters, and what is made of the sums v
   auto weights = [&](int r, int c) {
@@ -509,7 +529,7 @@ int run(gmi_instance* g, const gmi_muon* m, MuonArgs a, int steps) {
   muon_pack_kernel<F32><<<m->packs, 256, 0, g->stream>>>(a);
   GMI_LAUNCH_CHECK();
   for (int s = 0; s < steps; ++s) {
-    a.first = s == 0;
+    a.step = s;
     a.last = s == steps - 1;
     a.from = s & 1;
     a.to = 1 - a.from;

@@ -291,3 +291,34 @@ def test_refusals(inst):
     with pytest.raises(ValueError):
         g.muon_orthogonalize(inst, h, a.half(), b.half(), hp())
     g.gmi_muon_destroy(h)
+
+
+def steps64_of(u, steps, abc, eps=1e-7):
+    x = u / (u.norm() + eps)
+    for _ in range(steps):
+        s = x @ x.T
+        x = abc[0] * x + (abc[1] * s + abc[2] * (s @ s)) @ x
+    return x
+
+
+# entries of the first size or so; the norm is some 60 times that
+# (coefficients for 14 steps: ones that bring the singular values to 1 and hold them there)
+@pytest.mark.parametrize("steps,abc", [(1, ABC), (5, ABC), (14, (2.0, -1.5, 0.5))], ids=str)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size,eps", [(1e-6, 1e-7), (1e-9, 1e-7), (1e-12, 1e-7), (1e-14, 1e-7), (1e-18, 1e-7), (1e-24, 1e-7), (1e-3, 1.0), (3.0, 1e4),
+                                      (1e-20, 1e-20), (6e36, 1e-7), (3e37, 1e-7)])
+def test_gradients_of_any_size_relative_to_the_result(inst, size, eps, dtype, steps, abc):
+    """However little the division by |G| + eps leaves, and where the norm is beyond the type: the same relative error."""
+    import paper_2206_08482_amd as g
+    mats, total = layout([(40, 90), (90, 40)])
+    src = gradient(None, total, mats, TYPES[dtype], 3, size / 3)
+    assert torch.isfinite(src).all()
+    dst = torch.empty_like(src)
+    h = g.gmi_muon_bind(inst, mats, g.dtype_code(dtype))
+    torch.cuda.synchronize()
+    g.muon_orthogonalize(inst, h, src, dst, g.muon_hparams(steps=steps, eps=eps, a=abc[0], b=abc[1], c=abc[2]))
+    g.gmi_sync(inst)
+    for m in mats:
+        want = steps64_of(part(src, m).double().cpu(), steps, abc, float(torch.tensor(eps)))
+        assert rel(part(dst, m), want) <= TOL[dtype], m
+    g.gmi_muon_destroy(h)
