@@ -377,8 +377,9 @@ int grouped_linear_backward(gmi_t gmi, gmi_linear_t linear, const void* dy, int6
  *   m = momentum * m + g;  u = nesterov ? g + momentum * m : m;  W = (1 - lr * weight_decay) W - lr * sqrt(max(1, rows / cols)) * NS(u)
  * dtype F32: g, src and dst are fp32 and the products are of two fp16 planes per operand (22 bits of significand, three products).
  * dtype BF16: g, src and dst are bf16, one fp16 plane per operand (11 bits).  Sums in fp32; parameters and momentum are fp32 for both.
- * A zero matrix gives zero; one that holds an infinity or NaN gives NaN.  The fp16 planes hold b S + c S^2 up to a magnitude of 60 (10 with the
- * usual coefficients); coefficients that go beyond give NaN. */
+ * A zero matrix gives zero; one that holds an infinity or NaN gives NaN.  a, b, c: with p(s) = a + b s + c s^2 a step makes |p(v^2)| v of a singular value v,
+ * and values begin in 0 .. 1; coefficients with which 2 |p| in the first step, |p| or v^2 in a later one could pass 2^20 (10^6) are refused
+ * (GMI_ERR_INVALID_ARG).  The usual ones stay below 7 and 1.5. */
 typedef struct gmi_muon* gmi_muon_t;
 typedef struct {
   int32_t rows, cols;        /* 1 .. 32768, row-major */

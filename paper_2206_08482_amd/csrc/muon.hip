@@ -8,7 +8,9 @@
 // A bf16 gradient is held exactly by one plane of 11 bits (down to 2^-26 of the norm).  muon_update's direction u is fp32 and is rounded to those
 // 11 bits, once, with bf16 gradients: 2^-12 of it, beside the 2^-9 that the gradient itself was rounded to.
 //
-// Powers of two keep the fp16 values away from the ends of the type: entries of X and S reach 1 and may be as small as 1 / sqrt(p q).
+// Powers of two keep the fp16 values away from the ends of the type: entries of X and S reach 1 and may be as small as 1 / sqrt(p q).  What the coefficients
+// can make of singular values in 0 .. 1 bounds X, S and B in every step, and where a bound is larger the power is smaller: scales_of.
+#include <cmath>
 #include <numeric>
 
 #include "product.h"
@@ -21,7 +23,9 @@ constexpr uint32_t kMagicMuon = 0x474d4955;
 
 namespace {
 
-constexpr int kScaleX = 12, kScaleS = 10, kScaleB = 10;      // exponents of the stored X, S, B
+constexpr int kScaleX = 12, kScaleS = 10, kScaleB = 10;      // exponents of the stored X, S, B; smaller where these may leave fp16
+constexpr int kMostSteps = 64;
+struct Scales { int x, s, b; };      // of a step: of the X that it reads, of S, of B
 constexpr int kNormChunk = 2048, kMostChunks = 512;          // elements whose squares a workgroup sums at a time; workgroups of a matrix
 
 constexpr int kSides[4] = {256, 192, 128, 64};
@@ -73,6 +77,8 @@ struct MuonArgs {
   void* dst;
   float momentum, a, b, c, eps, lr, decay;
   int nesterov, step, last, from, to;       // of a step: X[from] -> X[to]
+  Scales scale;                             // of the step
+  int scale_to;                             // of the X that it writes
   int tile0, splits;                        // of the launch: place of its first tile in the running count
   float* part;                              // sums of splits, 64 x 64 of each workgroup
   Entry only;                               // the table's first
@@ -308,8 +314,8 @@ __global__ __launch_bounds__(S::threads, kWavesPerSimd<S>) void muon_symmetric_k
   }
 
   const Carry t = SQUARE ? carry_of(a, t0, a.step) : Carry{1.f, 1.f};
-  const float ta = t.with * a.a * (1 << kScaleB), tb = t.with * t.at * t.at * a.b * ldexpf(1.f, kScaleB - kScaleS),
-              tc = t.with * t.at * t.at * t.at * t.at * a.c * ldexpf(1.f, kScaleB - 2 * kScaleS), ts = ldexpf(1.f, kScaleS - 2 * kScaleX);
+  const float ta = t.with * a.a * ldexpf(1.f, a.scale.b), tb = t.with * t.at * t.at * a.b * ldexpf(1.f, a.scale.b - a.scale.s),
+              tc = t.with * t.at * t.at * t.at * t.at * a.c * ldexpf(1.f, a.scale.b - 2 * a.scale.s), ts = ldexpf(1.f, a.scale.s - 2 * a.scale.x);
   const char* s = a.base + E.s;
   char* out = a.base + (SQUARE ? E.b : E.s);
   // eight values of row m at columns n ..: S there, and what is made of the sums v
@@ -347,7 +353,7 @@ __global__ __launch_bounds__(256) void muon_join_kernel(MuonArgs a) {
   __shared__ float sums[T][T + 1];
   const TriangleTile tile = triangle_tile<T>(a, a.tile0 + blockIdx.x);
   const Entry& E = tile.E;
-  const float ts = ldexpf(1.f, kScaleS - 2 * kScaleX);
+  const float ts = ldexpf(1.f, a.scale.s - 2 * a.scale.x);
   char* out = a.base + E.s;
   const float* from = a.part + (int64_t)blockIdx.x * a.splits * (T * T);
 #pragma unroll
@@ -400,7 +406,7 @@ __global__ __launch_bounds__(S::threads, kWavesPerSimd<S>) void muon_apply_kerne
   multiply<S, true, false, true>(P, Q, E.p, F32 ? kTwoPlanes : kOnePlane, smem, acc);
 
   if (!a.last) {
-    const float scale = ldexpf(1.f, -kScaleB);
+    const float scale = ldexpf(1.f, a.scale_to - a.scale.x - a.scale.b);
     each_row<S>(acc, smem, FetchNothing(), [&](int m, int n, float (&v)[8], Nothing) {
       if (m0 + m >= E.p || n0 + n >= E.qp) return;
 #pragma unroll
@@ -410,7 +416,7 @@ __global__ __launch_bounds__(S::threads, kWavesPerSimd<S>) void muon_apply_kerne
     });
     return;
   }
-  const float scale = carry_of(a, t0, a.step + 1).at * ldexpf(1.f, -kScaleB - kScaleX);
+  const float scale = carry_of(a, t0, a.step + 1).at * ldexpf(1.f, -a.scale.b - a.scale.x);
   const float step = a.lr * sqrtf(fmaxf(1.f, (float)E.rows / (float)E.cols));
   // eight values of row r of the matrix at columns c ..: its parameters, and what is made of the sums v
   auto weights = [&](int r, int c) {
@@ -522,8 +528,39 @@ void plan_parts(gmi_muon* m, int product, int cus) {
   add(*second, cut, n);
 }
 
+// The scales of `steps` steps; false if X X^T or B may pass 2^20, which the planes' 2^15 and what small entries need of their other end are not made for.
+// A singular value in 0 .. most becomes v |p(v^2)| with p(s) = a + b s + c s^2 (that of X, not of the Y that carry_of speaks of, which is smaller), 1/64 of
+// it is left for roundings, a factor of 2 to fp16's largest.
+bool scales_of(const gmi_muon_hparams& hp, Scales (&out)[kMostSteps]) {
+  const double a = hp.a, b = hp.b, c = hp.c;
+  if (!(std::isfinite(a) && std::isfinite(b) && std::isfinite(c))) return false;
+  auto p = [&](double s) { return std::fabs(a + s * (b + s * c)); };
+  auto exponent = [](int most, double bound) {
+    while (std::ldexp(bound, most) > 32768.0) --most;
+    return most;
+  };
+  double most = 1.0;
+  for (int k = 0; k < hp.steps; ++k) {
+    const double s = most * most;
+    double of_b = std::max(p(0.0), p(s)), next = most * p(s);
+    if (c != 0.0 && -b / (2.0 * c) > 0.0 && -b / (2.0 * c) < s) of_b = std::max(of_b, p(-b / (2.0 * c)));
+    // where v p(v^2) is flat: a + 3 b s + 5 c s^2 = 0
+    const double root = 9.0 * b * b - 20.0 * a * c, q = -0.5 * (3.0 * b + std::copysign(std::sqrt(std::max(root, 0.0)), b));
+    for (const double at : {c != 0.0 ? q / (5.0 * c) : -1.0, q != 0.0 ? a / q : -1.0})
+      if (root >= 0.0 && at > 0.0 && at < s) next = std::max(next, std::sqrt(at) * p(at));
+    if (k == 0) of_b *= 2.0;      // the factor t of the first step
+    if (!(s <= 1048576.0 && of_b <= 1048576.0)) return false;
+    out[k] = {exponent(kScaleX, most), exponent(kScaleS, s), exponent(kScaleB, of_b)};
+    most = std::max(most, next * (1.0 + 1.0 / 64));
+  }
+  return true;
+}
+
 template <bool F32>
-int run(gmi_instance* g, const gmi_muon* m, MuonArgs a, int steps) {
+int run(gmi_instance* g, const gmi_muon* m, MuonArgs a, const char* who, const gmi_muon_hparams& hp) {
+  const int steps = hp.steps;
+  Scales scales[kMostSteps];
+  if (!scales_of(hp, scales)) GMI_FAIL(GMI_ERR_INVALID_ARG, "%s: coefficients %g, %g, %g may lengthen a matrix beyond what %d steps hold", who, hp.a, hp.b, hp.c, steps);
   muon_norm_kernel<F32><<<m->chunks, 256, 0, g->stream>>>(a);
   GMI_LAUNCH_CHECK();
   muon_pack_kernel<F32><<<m->packs, 256, 0, g->stream>>>(a);
@@ -533,6 +570,8 @@ int run(gmi_instance* g, const gmi_muon* m, MuonArgs a, int steps) {
     a.last = s == steps - 1;
     a.from = s & 1;
     a.to = 1 - a.from;
+    a.scale = scales[s];
+    a.scale_to = a.last ? 0 : scales[s + 1].x;
     for (int product = 0; product < 3; ++product)
       for (const Part& part : m->parts[product]) {
         a.tile0 = part.first;
@@ -556,7 +595,7 @@ int check_muon(const char* who, gmi_t g, gmi_muon_t m, const gmi_muon_hparams* h
   if (!valid(m)) GMI_FAIL(GMI_ERR_BAD_HANDLE, "%s: bad binding", who);
   if (g->device != m->device) GMI_FAIL(GMI_ERR_INVALID_ARG, "%s: instance and binding live on different devices", who);
   if (!hp) GMI_FAIL(GMI_ERR_INVALID_ARG, "%s: hp is NULL", who);
-  if (hp->steps < 1 || hp->steps > 64) GMI_FAIL(GMI_ERR_INVALID_ARG, "%s: steps %d outside 1 .. 64", who, hp->steps);
+  if (hp->steps < 1 || hp->steps > kMostSteps) GMI_FAIL(GMI_ERR_INVALID_ARG, "%s: steps %d outside 1 .. %d", who, hp->steps, kMostSteps);
   if (!(hp->eps > 0.f)) GMI_FAIL(GMI_ERR_INVALID_ARG, "%s: eps has to be positive", who);
   return GMI_OK;
 }
@@ -691,7 +730,7 @@ extern "C" int muon_orthogonalize(gmi_t g, gmi_muon_t m, const void* src, void* 
   MuonArgs a = args_of(m, hp);
   a.src = src;
   a.dst = dst;
-  return m->dtype == GMI_DTYPE_F32 ? run<true>(g, m, a, hp->steps) : run<false>(g, m, a, hp->steps);
+  return m->dtype == GMI_DTYPE_F32 ? run<true>(g, m, a, "muon_orthogonalize", *hp) : run<false>(g, m, a, "muon_orthogonalize", *hp);
 }
 
 extern "C" int muon_update(gmi_t g, gmi_muon_t m, const float* params, const float* moments, const void* grad, const gmi_muon_hparams* hp,
@@ -714,5 +753,5 @@ extern "C" int muon_update(gmi_t g, gmi_muon_t m, const float* params, const flo
   a.moments = moments;
   a.params_out = params_out;
   a.moments_out = moments_out;
-  return m->dtype == GMI_DTYPE_F32 ? run<true>(g, m, a, hp->steps) : run<false>(g, m, a, hp->steps);
+  return m->dtype == GMI_DTYPE_F32 ? run<true>(g, m, a, "muon_update", *hp) : run<false>(g, m, a, "muon_update", *hp);
 }

@@ -322,3 +322,57 @@ def test_gradients_of_any_size_relative_to_the_result(inst, size, eps, dtype, st
         want = steps64_of(part(src, m).double().cpu(), steps, abc, float(torch.tensor(eps)))
         assert rel(part(dst, m), want) <= TOL[dtype], m
     g.gmi_muon_destroy(h)
+
+
+def concentrated(r, c, type_, seed):
+    """A matrix of rank one: its one singular value is its norm."""
+    gen = torch.Generator().manual_seed(seed)
+    return (torch.randn(r, 1, generator=gen, dtype=torch.float64) @ torch.randn(1, c, generator=gen, dtype=torch.float64)).to(type_)
+
+
+# (coefficients, steps): singular values that reach 20, 400; 47 and, from there, 5e6; 60 after 100 at small ones
+COEFFICIENTS = [((20.0, 0.0, 0.0), 2), ((20.0, 0.0, 0.0), 3), ((3.4445, -50.0, 0.0), 1), ((3.4445, -50.0, 0.0), 2), ((100.0, -50.0, 10.0), 1)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("abc,steps", COEFFICIENTS, ids=str)
+def test_coefficients_that_lengthen(inst, abc, steps, dtype):
+    """The largest singular value there can be, the norm itself.  With a = 3.4445, b = -50 a step multiplies relative errors by up to 3; the
+    tolerances hold roundings of the planes by 4 (2^-12 each, 2^-22 in fp32) several times over, twice so for two such steps."""
+    import paper_2206_08482_amd as g
+    shapes = [(1, 1), (33, 70), (130, 20), (200, 200)]
+    mats, total = layout(shapes)
+    src = torch.zeros(total, dtype=TYPES[dtype])
+    for i, (r, c, o) in enumerate(mats):
+        src[o:o + r * c] = concentrated(r, c, TYPES[dtype], 20 + i).flatten()
+    src = src.cuda()
+    dst = torch.full_like(src, 5.0)
+    h = g.gmi_muon_bind(inst, mats, g.dtype_code(dtype))
+    torch.cuda.synchronize()
+    g.muon_orthogonalize(inst, h, src, dst, g.muon_hparams(steps=steps, a=abc[0], b=abc[1], c=abc[2]))
+    g.gmi_sync(inst)
+    for m in mats:
+        want = steps64_of(part(src, m).double().cpu(), steps, abc)
+        assert rel(part(dst, m), want) <= TOL[dtype] * (2 if steps == 2 else 1), m
+    g.gmi_muon_destroy(h)
+
+
+def test_coefficients_beyond_the_planes_are_refused(inst):
+    import paper_2206_08482_amd as g
+    h = g.gmi_muon_bind(inst, [(4, 4, 0)], g.DTYPE_F32)
+    src = torch.eye(4, device="cuda").flatten()
+    dst, moments, params = torch.full_like(src, 5.0), torch.zeros_like(src), torch.ones_like(src)
+    torch.cuda.synchronize()
+    nan = float("nan")
+    for kw in (dict(a=2000.0, b=0.0, c=0.0, steps=3), dict(b=-50.0, c=0.0, steps=4), dict(a=1e30), dict(c=1e38), dict(a=nan), dict(b=nan), dict(c=float("inf"))):
+        hp = g.muon_hparams(**kw)
+        for call in (lambda: g.muon_orthogonalize(inst, h, src, dst, hp), lambda: g.muon_update(inst, h, params, moments, src, hp)):
+            with pytest.raises(g.GmiError) as e:
+                call()
+            assert e.value.code == g.ERR_INVALID_ARG, kw
+    g.gmi_sync(inst)
+    assert (dst == 5.0).all() and (params == 1.0).all() and (moments == 0.0).all()
+    g.muon_orthogonalize(inst, h, src, dst, g.muon_hparams(a=2000.0, b=0.0, c=0.0, steps=1))      # the last step's result is not kept in planes
+    g.gmi_sync(inst)
+    assert torch.allclose(dst, 1000.0 * src, rtol=1e-5)
+    g.gmi_muon_destroy(h)
