@@ -361,7 +361,8 @@ int linear_backward(gmi_t gmi, gmi_linear_t linear, const void* dy, int64_t lddy
                     const void* pre, int64_t ldp, int32_t n_rows, void* dx, int64_t lddx, void* dw, float* dbias);
 /* The same with rows offsets[g] .. offsets[g+1]-1 in group g; offsets dev i32 [n_groups + 1], ascending, within 0 .. n_rows
  * (read on the device; values outside are cut to that range).  Rows of no group are neither read nor written; a group without rows has
- * dw = 0, dbias = 0. */
+ * dw = 0, dbias = 0.  A call with more tiles than a launch has workgroups (2^22 tiles of 256 x 256 with each group's last ones counted whole; for dz and
+ * dbias 2^24 tiles of rows of a group x 256) is refused with GMI_ERR_BAD_SHAPE before anything is written. */
 int grouped_linear_forward(gmi_t gmi, gmi_linear_t linear, const void* x, int64_t ldx, const int32_t* offsets, const void* w,
                            const float* bias, const void* residual, int64_t ldr, int32_t n_rows, void* y, int64_t ldy,
                            void* pre, int64_t ldp);

@@ -24,6 +24,8 @@ namespace {
 constexpr int kSlopeRows = 8, kSlopeRowsMost = 256;  // rows of a group whose dz a workgroup forms and sums
 constexpr int64_t kPartBytes = (int64_t)64 << 20;    // most room for the sums of splits
 constexpr int kMostSplits = 64;
+// A launch has less than 2^32 threads: workgroups of any of the kernels (up to 1024 threads), of linear_prepare_kernel.
+constexpr int64_t kMostBlocks = ((int64_t)1 << 22) - 1, kMostPrepareBlocks = ((int64_t)1 << 24) - 1;
 
 inline bool valid(gmi_linear_t l) { return l && l->magic == gmi::kMagicLinear; }
 inline int pad8(int v) { return (v + 7) & ~7; }
@@ -453,7 +455,10 @@ __device__ __forceinline__ void bias_block(const BiasJob& j, const Groups& group
 }
 __global__ __launch_bounds__(1024) void linear_bias_kernel(BiasJob j, Groups groups) {
   __shared__ float sums[1024];
-  bias_block<1024>(j, groups, blockIdx.x, sums);
+  for (int b = blockIdx.x; b < j.blocks; b += gridDim.x) {
+    bias_block<1024>(j, groups, b, sums);
+    __syncthreads();
+  }
 }
 
 // The backward pass's two products and the bias's sums, which all read dz, in one launch: what one leaves of the chip idle the next takes.
@@ -519,6 +524,9 @@ struct Work {      // a product to plan
 Work work_of(const gmi_linear* l, const ProductArgs& a, int form, int64_t depth) {
   return {form == kWeightGrad ? a.rows : a.groups.rows, a.cols, depth, a.pairs.n, a.groups.n, form, l->part_bytes};
 }
+int64_t blocks_of(const Work& w, int shape, int splits) {
+  return tiles_of(w.rows, w.cols, w.groups, kTiles[shape].size, w.form == kWeightGrad) * splits;
+}
 // Of a product with tile i and s splits: us of a compute unit in all, of its longest workgroup (which shares its unit if there are that many),
 // and of joining the splits.  sum < 0: not to be had.
 struct Cost { float sum, longest, join, rounds; };
@@ -531,6 +539,7 @@ Cost cost_of(const gmi_instance* g, const Work& w, int i, int s) {
                                     : tiles_of(w.rows, w.cols, 1, tile.size, false) +
                                           (w.groups > 1 ? w.groups / 2 * ((w.cols + tile.size[1] - 1) / tile.size[1]) : 0));
   if (s > 1 && (w.depth < 64 * s || bytes * s > w.room || tiles > 4 * cus)) return {-1.f, 0.f, 0.f, 0.f};
+  if (blocks_of(w, i, s) > kMostBlocks) return {-1.f, 0.f, 0.f, 0.f};
   const float unit = tile_time(tile, (float)(w.depth * w.products) / s), alone = tile.alone * unit;
   Cost c;
   c.sum = (float)tiles / cus * unit;
@@ -542,11 +551,12 @@ Cost cost_of(const gmi_instance* g, const Work& w, int i, int s) {
   if (w.groups > 1) c.rounds = std::max(c.longest, c.sum + 0.35f * c.longest);
   return c;
 }
-// The tile and the number of splits of the contraction that take least by these figures.
+constexpr float kNever = 1e30f;
+// The tile and the number of splits of the contraction that take least by these figures.  *time kNever: more workgroups than a launch has, with any.
 Plan plan_product(const gmi_instance* g, const Work& w, float* time) {
   const int n_tiles = w.form == kForward ? 7 : w.form == kInputGrad ? 5 : 4;      // those built for the form
   Plan best = {0, 1};
-  *time = 1e30f;
+  *time = kNever;
   for (int i = 0; i < n_tiles; ++i)
     for (int s = 1; s <= kMostSplits; s *= 2) {
       const Cost c = cost_of(g, w, i, s);
@@ -556,14 +566,14 @@ Plan plan_product(const gmi_instance* g, const Work& w, float* time) {
     }
   return best;
 }
-// Both products of a backward pass with one tile (weight gradients in s splits) in one launch.
-Plan plan_gradients(const gmi_instance* g, const Work& x, const Work& w, float* time) {
+// Both products of a backward pass with one tile (weight gradients in s splits) in one launch, beside `others` workgroups.
+Plan plan_gradients(const gmi_instance* g, const Work& x, const Work& w, int64_t others, float* time) {
   Plan best = {0, 1};
-  *time = 1e30f;
+  *time = kNever;
   for (int i = 0; i < 4; ++i)
     for (int s = 1; s <= kMostSplits; s *= 2) {
       const Cost cx = cost_of(g, x, i, 1), cw = cost_of(g, w, i, s);
-      if (cw.sum < 0.f) break;
+      if (cx.sum < 0.f || cw.sum < 0.f || blocks_of(x, i, 1) + blocks_of(w, i, s) + others > kMostBlocks) break;
       const float share = (cx.sum > 0.5f * cx.longest ? kTiles[i].share : 1);      // the weights' workgroups run beside the others
       const float t = kStart + std::max(std::max(cx.longest, cw.longest * share), cx.sum + cw.sum + 0.5f * cx.longest) + cw.join;
       if (t < *time) { *time = t; best = {i, s}; }
@@ -591,7 +601,6 @@ int launch_join(gmi_instance* g, const ProductArgs& a) {
 int64_t blocks_of(const ProductArgs& a, bool weight, const Plan& p) {
   return tiles_of(weight ? a.rows : a.groups.rows, a.cols, a.groups.n, kTiles[p.shape].size, weight) * p.splits;
 }
-constexpr int64_t kMostBlocks = ((int64_t)1 << 22) - 1;      // a launch has less than 2^32 threads
 
 // Whether an output's lines are stored as ones that L2 need not keep: less is left to be written back when the launch ends.  16384 x 512 -> 512
 // with z kept (32 MiB) 20.0 -> 17.9 us, input gradients of 4096 x 1024 x 1024 (8 MiB) 17.2 -> 15.3, the backward pass of 16384 rows over 8 experts
@@ -608,11 +617,10 @@ int run_raw(gmi_instance* g, const ProductArgs& a, const Plan& p) {
 }
 
 template <int FORM, bool F32>
-int run_product(gmi_instance* g, const char* who, ProductArgs a, const Plan& p) {
+int run_product(gmi_instance* g, ProductArgs a, const Plan& p) {
   constexpr bool weight = FORM == kWeightGrad;
   a.splits = p.splits;
   const int64_t blocks = blocks_of(a, weight, p);
-  if (blocks > kMostBlocks) GMI_FAIL(GMI_ERR_BAD_SHAPE, "%s: %lld tiles", who, (long long)blocks);
   if (blocks == 0) return GMI_OK;
   int rc;
   switch (p.shape) {
@@ -643,12 +651,11 @@ int launch_gradients(gmi_instance* g, const ProductArgs& x, int64_t x_blocks, co
 }
 // weights NULL: the input gradients and the bias's sums alone.
 template <bool F32>
-int run_gradients(gmi_instance* g, const char* who, ProductArgs x, const ProductArgs* weights, const BiasJob& bias, const Plan& p) {
+int run_gradients(gmi_instance* g, ProductArgs x, const ProductArgs* weights, const BiasJob& bias, const Plan& p) {
   x.splits = 1;
   ProductArgs w = weights ? *weights : x;
   w.splits = p.splits;
   const int64_t xb = blocks_of(x, false, {p.shape, 1}), wb = weights ? blocks_of(w, true, p) : 0;
-  if (xb + wb + bias.blocks > kMostBlocks) GMI_FAIL(GMI_ERR_BAD_SHAPE, "%s: %lld tiles", who, (long long)(xb + wb));
   const int rc = p.shape == 0   ? launch_gradients<Large, F32>(g, x, xb, w, wb, bias)
                  : p.shape == 1 ? launch_gradients<Medium, F32>(g, x, xb, w, wb, bias)
                  : p.shape == 2 ? launch_gradients<Small, F32>(g, x, xb, w, wb, bias) : launch_gradients<Twin, F32>(g, x, xb, w, wb, bias);
@@ -731,6 +738,7 @@ int forward(const char* who, gmi_t g, gmi_linear_t l, const void* x, int64_t ldx
   a.once = stored_once(y, ldy, F32 ? 4 : 2, (int64_t)n_rows * d.out_dim * (F32 ? 4 : 2) * (pre ? 2 : 1));
   float time;
   const Plan plan = plan_product(g, work_of(l, a, kForward, Kp), &time);
+  if (time >= kNever) GMI_FAIL(GMI_ERR_BAD_SHAPE, "%s: more tiles than a launch has workgroups", who);
   const bool x_fits = in_place(l, X), w_fits = in_place(l, W);
   // A packed copy is a launch of its own, and one of w reads and writes all groups' weights.  Through registers w goes into as many tiles as
   // there are 16 rows: 1 x 4097 -> 4096 23 -> 13.4 us, 64 x 4097 -> 1024 16.2 -> 13.3, 16 rows over 64 experts of 4001 -> 4096 886 -> 14;
@@ -749,7 +757,7 @@ int forward(const char* who, gmi_t g, gmi_linear_t l, const void* x, int64_t ldx
     GMI_LAUNCH_CHECK();
   }
   a.p_group = a.p_ld * d.out_dim;
-  return run_product<kForward, F32>(g, who, a, plan);
+  return run_product<kForward, F32>(g, a, plan);
 }
 
 int forward_call(const char* who, bool grouped, gmi_t g, gmi_linear_t l, const void* x, int64_t ldx, const int32_t* offsets, const void* w,
@@ -799,12 +807,6 @@ int backward(const char* who, gmi_t g, gmi_linear_t l, const void* dy, int64_t l
                 d.out_dim, d.act, (int)(tiles * across), across};
     if (stored) { zp = l->dz; z_ld = Np * 2; }
   }
-  const int64_t blocks = (int64_t)pa.slope.blocks + pa.pack[0].blocks + pa.pack[1].blocks;
-  if (tiles * across > kMostBlocks) GMI_FAIL(GMI_ERR_BAD_SHAPE, "%s: %lld row tiles", who, (long long)(tiles * across));
-  if (blocks) {
-    linear_prepare_kernel<F32><<<dim3((unsigned)blocks), 256, 0, g->stream>>>(pa);
-    GMI_LAUNCH_CHECK();
-  }
   ProductArgs a = {};
   a.groups = G;
   a.pairs = pairs;
@@ -822,21 +824,27 @@ int backward(const char* who, gmi_t g, gmi_linear_t l, const void* dy, int64_t l
   bw.out = dw; bw.ldo = d.in_dim;
   bw.once = stored_once(dw, d.in_dim, F32 ? 4 : 2, (int64_t)groups * d.out_dim * d.in_dim * (F32 ? 4 : 2));
   const Work wx = work_of(l, bx, kInputGrad, d.out_dim), ww = work_of(l, bw, kWeightGrad, n_rows / groups);
-  float tx = 0.f, tw = 0.f, both = 1e30f;
+  float tx = 0.f, tw = 0.f, both = kNever;
   const bool have_x = dx && n_rows;
   const Plan px = have_x ? plan_product(g, wx, &tx) : Plan(), pw = dw ? plan_product(g, ww, &tw) : Plan();
   Plan pb = {};
-  if (have_x && dw) pb = plan_gradients(g, wx, ww, &both);
-  if (both <= tx + tw + (bias.blocks ? kStart : 0.f)) return run_gradients<F32>(g, who, bx, &bw, bias, pb);
-  if (have_x && bias.blocks && px.shape < 4 && px.splits == 1) {
-    LINEAR_TRY(run_gradients<F32>(g, who, bx, nullptr, bias, px));
+  if (have_x && dw) pb = plan_gradients(g, wx, ww, bias.blocks, &both);
+  const int64_t blocks = (n_rows && (stored || dbias) ? tiles * across : 0) + pa.pack[0].blocks + pa.pack[1].blocks;
+  if (tx >= kNever || tw >= kNever || blocks > kMostPrepareBlocks) GMI_FAIL(GMI_ERR_BAD_SHAPE, "%s: more tiles than a launch has workgroups", who);
+  if (blocks) {
+    linear_prepare_kernel<F32><<<dim3((unsigned)blocks), 256, 0, g->stream>>>(pa);
+    GMI_LAUNCH_CHECK();
+  }
+  if (both <= tx + tw + (bias.blocks ? kStart : 0.f)) return run_gradients<F32>(g, bx, &bw, bias, pb);
+  if (have_x && bias.blocks && px.shape < 4 && px.splits == 1 && blocks_of(bx, false, px) + bias.blocks <= kMostBlocks) {
+    LINEAR_TRY(run_gradients<F32>(g, bx, nullptr, bias, px));
     bias.blocks = 0;
   } else if (have_x) {
-    LINEAR_TRY((run_product<kInputGrad, F32>(g, who, bx, px)));
+    LINEAR_TRY((run_product<kInputGrad, F32>(g, bx, px)));
   }
-  if (dw) LINEAR_TRY((run_product<kWeightGrad, F32>(g, who, bw, pw)));
+  if (dw) LINEAR_TRY((run_product<kWeightGrad, F32>(g, bw, pw)));
   if (bias.blocks) {
-    linear_bias_kernel<<<dim3((unsigned)bias.blocks), 1024, 0, g->stream>>>(bias, G);
+    linear_bias_kernel<<<dim3((unsigned)std::min<int64_t>(bias.blocks, kMostBlocks)), 1024, 0, g->stream>>>(bias, G);
     GMI_LAUNCH_CHECK();
   }
   return GMI_OK;
