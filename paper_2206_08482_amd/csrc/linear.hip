@@ -774,10 +774,11 @@ int forward_call(const char* who, bool grouped, gmi_t g, gmi_linear_t l, const v
   const int64_t groups = std::max(1, d.n_groups);
   const Span sx = span_of(l, x, n_rows, d.in_dim, ldx), sw = span_of(l, w, groups * d.out_dim, d.in_dim, d.in_dim),
              sr = span_of(l, residual, n_rows, d.out_dim, ldr), sy = span_of(l, y, n_rows, d.out_dim, ldy),
-             sp = span_of(l, pre, n_rows, d.out_dim, ldp), sb = span_of(l, bias, groups, d.out_dim, d.out_dim, 4);
+             sp = span_of(l, pre, n_rows, d.out_dim, ldp), sb = span_of(l, bias, groups, d.out_dim, d.out_dim, 4),
+             so = span_of(l, offsets, 1, groups + 1, groups + 1, 4);
   const bool same = residual == y && ldr == ldy;
   if (overlap(sy, sx) || overlap(sy, sw) || (!same && overlap(sy, sr)) || overlap(sy, sp) || overlap(sy, sb) || overlap(sp, sx) ||
-      overlap(sp, sw) || overlap(sp, sr) || overlap(sp, sb))
+      overlap(sp, sw) || overlap(sp, sr) || overlap(sp, sb) || overlap(sy, so) || overlap(sp, so))
     GMI_FAIL(GMI_ERR_INVALID_ARG, "%s: an output overlaps another argument", who);
   return d.dtype == GMI_DTYPE_F32
              ? forward<true>(who, g, l, x, ldx, offsets, w, bias, residual, ldr, n_rows, y, ldy, pre, ldp)
@@ -865,9 +866,9 @@ int backward_call(const char* who, bool grouped, gmi_t g, gmi_linear_t l, const 
   LINEAR_TRY(check_matrix(who, "dw", l, dw, d.in_dim, d.in_dim, false));
   if ((uintptr_t)dbias % 4) GMI_FAIL(GMI_ERR_INVALID_ARG, "%s: dbias is not aligned", who);
   const int64_t groups = std::max(1, d.n_groups);
-  const Span in[4] = {span_of(l, dy, n_rows, d.out_dim, lddy), span_of(l, dw ? x : nullptr, n_rows, d.in_dim, ldx),
+  const Span in[5] = {span_of(l, dy, n_rows, d.out_dim, lddy), span_of(l, dw ? x : nullptr, n_rows, d.in_dim, ldx),
                       span_of(l, dx ? w : nullptr, groups * d.out_dim, d.in_dim, d.in_dim),
-                      span_of(l, d.act != GMI_ACT_NONE ? pre : nullptr, n_rows, d.out_dim, ldp)};
+                      span_of(l, d.act != GMI_ACT_NONE ? pre : nullptr, n_rows, d.out_dim, ldp), span_of(l, offsets, 1, groups + 1, groups + 1, 4)};
   const Span out[3] = {span_of(l, dx, n_rows, d.in_dim, lddx), span_of(l, dw, groups * d.out_dim, d.in_dim, d.in_dim),
                        span_of(l, dbias, groups, d.out_dim, d.out_dim, 4)};
   for (int i = 0; i < 3; ++i) {
