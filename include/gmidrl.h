@@ -334,8 +334,10 @@ int adam_update(gmi_t gmi, float* params, float* adam_m, float* adam_v, const fl
  * Shapes: x [n_rows, in_dim], w [out_dim, in_dim] (grouped: [n_groups, out_dim, in_dim]), bias [out_dim] ([n_groups, out_dim]),
  * y, pre, residual, dy [n_rows, out_dim], dx as x, dw as w, dbias as bias; w, bias, dw, dbias contiguous, the others with a row pitch
  * ld* (elements, >= the row's length).  Any pitch and any element-aligned address is right; 16-byte aligned rows whose length is a
- * multiple of 8 are read in place (bf16), others through a packed copy in the binding's workspace.  That holds a packed x and w, with
- * `backward` a dz, and up to 64 MiB for the partial sums of products with few outputs and a long contraction. */
+ * multiple of 8 are read in place (bf16; a forward pass of few rows, at most 64 a group, may read any rows where they lie), others through
+ * a packed copy in the binding's workspace.  That holds room for a packed x and w, with `backward` for a dz, and up to 64 MiB for the
+ * partial sums of products with few outputs and a long contraction, whether or not a call needs them: with n_groups large matrices as
+ * much as w itself. */
 typedef enum { GMI_ACT_NONE = 0, GMI_ACT_ELU = 1, GMI_ACT_RELU = 2, GMI_ACT_SILU = 3, GMI_ACT_GELU = 4 } gmi_activation;   /* GELU: z Phi(z) */
 typedef struct gmi_linear* gmi_linear_t;
 typedef struct {
@@ -360,9 +362,10 @@ int linear_forward(gmi_t gmi, gmi_linear_t linear, const void* x, int64_t ldx, c
 int linear_backward(gmi_t gmi, gmi_linear_t linear, const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* w,
                     const void* pre, int64_t ldp, int32_t n_rows, void* dx, int64_t lddx, void* dw, float* dbias);
 /* The same with rows offsets[g] .. offsets[g+1]-1 in group g; offsets dev i32 [n_groups + 1], ascending, within 0 .. n_rows
- * (read on the device; values outside are cut to that range).  Rows of no group are neither read nor written; a group without rows has
- * dw = 0, dbias = 0.  A call with more tiles than a launch has workgroups (2^22 tiles of 256 x 256 with each group's last ones counted whole; for dz and
- * dbias 2^24 tiles of rows of a group x 256) is refused with GMI_ERR_BAD_SHAPE before anything is written. */
+ * (read on the device; values outside are cut to that range).  Rows of no group are not written, and what they hold has no effect (a
+ * packed copy of x reads them); a group without rows has dw = 0, dbias = 0.  A call with more tiles than a launch has workgroups (2^22
+ * tiles of 256 x 256, each group's last ones counted whole; for dz and dbias 2^24 tiles of a group's rows x 256) is refused with
+ * GMI_ERR_BAD_SHAPE before anything is written. */
 int grouped_linear_forward(gmi_t gmi, gmi_linear_t linear, const void* x, int64_t ldx, const int32_t* offsets, const void* w,
                            const float* bias, const void* residual, int64_t ldr, int32_t n_rows, void* y, int64_t ldy,
                            void* pre, int64_t ldp);
@@ -394,7 +397,8 @@ typedef struct {
   float eps;                             /* > 0, commonly 1e-7 */
 } gmi_muon_hparams;
 
-/* matrices host [n], 1 .. 4096 of them, not overlapping (copied).  Allocates the workspace of all of them. */
+/* matrices host [n], 1 .. 4096 of them, not overlapping (copied).  Allocates the workspace of all of them.  Calls through one binding share
+ * it: they belong on one stream. */
 int gmi_muon_bind(gmi_t gmi, const gmi_matrix* matrices, int32_t n, int32_t dtype, gmi_muon_t* out);
 int gmi_muon_destroy(gmi_muon_t muon);
 /* dst = NS(src) for every bound matrix; src, dst dev flat vectors of the binding's dtype, other elements are not touched.  dst may be
