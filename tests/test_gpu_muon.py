@@ -376,3 +376,26 @@ def test_coefficients_beyond_the_planes_are_refused(inst):
     g.gmi_sync(inst)
     assert torch.allclose(dst, 1000.0 * src, rtol=1e-5)
     g.gmi_muon_destroy(h)
+
+
+@pytest.mark.parametrize("cus", [8, 104])
+def test_instances_of_some_compute_units(inst, cus):
+    """Tiles and divisions of the contraction are planned for the binding's instance; another one may call it."""
+    import paper_2206_08482_amd as g
+    from paper_2206_08482_amd.instances import cu_masks
+    few = g.gmi_create(cu_masks(256, [cus])[0])
+    shapes = [(600, 600), (17, 3568), (211, 512), (90, 40)]
+    mats, total = layout(shapes)
+    for dtype in ("f32", "bf16"):
+        src = gradient(shapes, total, mats, TYPES[dtype], 12)
+        h = g.gmi_muon_bind(few, mats, g.dtype_code(dtype))
+        for caller in (few, inst):
+            dst = torch.full_like(src, 5.0)
+            torch.cuda.synchronize()
+            g.muon_orthogonalize(caller, h, src, dst, g.muon_hparams(steps=3))
+            g.gmi_sync(caller)
+            for m in mats:
+                assert rel(part(dst, m), steps64(part(src, m).double().cpu(), 3)) <= TOL[dtype], m
+            assert (dst.cpu()[outside(total, mats)] == 5.0).all()
+        g.gmi_muon_destroy(h)
+    g.gmi_destroy(few)
