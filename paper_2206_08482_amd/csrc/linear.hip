@@ -329,9 +329,9 @@ __device__ __forceinline__ void load_bias(const ProductArgs& a, int group, int c
 }
 
 // Workgroup `block` of a product: y = act(x w^T + b) + r, dx = dz w or dw = dz^T x; the tile comes from the place alone, the group from the
-// offsets.  Bound by the matrix cores at the card's power limit with whole 256 x 256 tiles (4096 x 8192 x 4096 204 us, 1.35 PFLOP/s; 8192 x 4096 x
-// 4096 with residual and z kept 240, of which the epilogue's 192 MiB take about 40 on their own), by memory with few rows (1 x 4096 -> 4096
-// 7.5 us, 4.5 TB/s), by the address units' 64 bytes a cycle and compute unit with 64 x 64 tiles.
+// offsets.  Bound by the matrix cores at the card's power limit with whole 256 x 256 tiles (4096 x 8192 x 4096 192 to 204 us, 1.35 to 1.43 PFLOP/s;
+// 8192 x 4096 x 4096 206, with GELU, residual and z kept 232 to 239: the epilogue's 192 MiB are about 30 of it), by memory with few rows (1 x 4096 ->
+// 4096 7.5 us, 4.5 TB/s), by the address units' 64 bytes a cycle and compute unit with 64 x 64 tiles.
 template <class S, int FORM, bool F32>
 __device__ __forceinline__ void product_block(const ProductArgs& a, int block, char* smem) {
   constexpr int TN = S::TN, TM = S::TM;
