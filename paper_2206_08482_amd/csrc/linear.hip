@@ -31,7 +31,8 @@ inline bool valid(gmi_linear_t l) { return l && l->magic == gmi::kMagicLinear; }
 inline int pad8(int v) { return (v + 7) & ~7; }
 
 // ------------------------------------------------------------------ activations
-// EXACT (fp32 layers): the library's functions.  Otherwise the hardware's exponential and reciprocal, 1e-7 .. 3e-7 of their value.
+// EXACT (fp32 layers): the library's functions.  Otherwise the hardware's exponential and reciprocal, 1e-7 .. 3e-7 of their value and, for the exponential,
+// 6e-8 |z| of it more (its argument's rounding); what is below 2^-126 becomes 0.
 template <bool EXACT>
 __device__ __forceinline__ float exp_of(float z) { return EXACT ? expf(z) : __builtin_amdgcn_exp2f(z * 1.44269504f); }
 template <bool EXACT>

@@ -529,8 +529,8 @@ void plan_parts(gmi_muon* m, int product, int cus) {
 }
 
 // The scales of `steps` steps; false if X X^T or B may pass 2^20, which the planes' 2^15 and what small entries need of their other end are not made for.
-// A singular value in 0 .. most becomes v |p(v^2)| with p(s) = a + b s + c s^2 (that of X, not of the Y that carry_of speaks of, which is smaller), 1/64 of
-// it is left for roundings, a factor of 2 to fp16's largest.
+// A singular value in 0 .. most becomes v |p(v^2)| with p(s) = a + b s + c s^2 (that of X, not of the Y that carry_of speaks of, which is smaller), 1/256 of
+// it is left for roundings (2^-11 each at the most), a factor of 2 to fp16's largest.
 bool scales_of(const gmi_muon_hparams& hp, Scales (&out)[kMostSteps]) {
   const double a = hp.a, b = hp.b, c = hp.c;
   if (!(std::isfinite(a) && std::isfinite(b) && std::isfinite(c))) return false;
@@ -551,7 +551,7 @@ bool scales_of(const gmi_muon_hparams& hp, Scales (&out)[kMostSteps]) {
     if (k == 0) of_b *= 2.0;      // the factor t of the first step
     if (!(s <= 1048576.0 && of_b <= 1048576.0)) return false;
     out[k] = {exponent(kScaleX, most), exponent(kScaleS, s), exponent(kScaleB, of_b)};
-    most = std::max(most, next * (1.0 + 1.0 / 64));
+    most = std::max(most, next * (1.0 + 1.0 / 256));
   }
   return true;
 }
